@@ -843,7 +843,8 @@ CrossShape cross_shape(const pbsa_cross& p, bool masked) {
     // 21.7, to 2000 41 and 123.  Two heads of 32 rows to 32760 states: 15.9 by states (16; by rows, on two compute units, 518).
     const double by_rows = 6.0 + (double)(((int64_t)p.Nk + 63) / 64) + (masked ? 4.0 : 0.0), groups = (double)(k.units * k.parts);
     const double by_keys = std::max(1.0, groups / kFill) * (5.0 + 1.6 * (double)turns / k.parts) + (k.parts > 1 ? 4.0 + groups / 60.0 : 0.0);
-    const bool far = masked && (int64_t)p.Nk * 2 * std::max(p.k[2], p.v[2]) >= ((int64_t)1 << 32);   // (Gather)
+    // Gather counts the bytes from the first state to a load of a listed one in 32 bits
+    const bool far = masked && ((int64_t)p.Nk - 1) * 2 * std::max(p.k[2], p.v[2]) + kGatherSpan > ((int64_t)1 << 32);
     if (far || (s.units < kFill && by_keys < by_rows)) s = k;
   }
   return s;

@@ -176,7 +176,8 @@ struct Loads {
 // The loads of N KiB of a tile of 64 states, from row r0 on (a multiple of 16), by one wave: states 64 i .. of the first `count`,
 // or of the list, whose next places lie in LDS (Picked).  States past the last one are not fetched: the last one stands in for
 // them.  Offsets are 32 bits wide, from the tile's first row, or with a list from the first state (a call whose states lie further
-// apart takes cross_keys_kernel).
+// apart takes cross_keys_kernel: cross_shape).
+constexpr int64_t kGatherSpan = 4096;      // more than a load's last byte lies behind its state's first: 256 of the row, 3 KiB (at)
 struct Picked {
   int32_t at[4][64];         // of tiles i mod 4
 };

@@ -32,3 +32,23 @@ def test_forward(case):
     assert ref.worst(o, r.o, r.o_tol) <= 1
     assert ref.worst(lse, r.lse, r.lse_tol) <= 1
     untouched(whole)
+
+
+@pytest.mark.parametrize("n_k", [128, 129])
+def test_masked_states_far_apart_in_memory(n_k):
+    """Few states, so far apart that a list's offsets fill 32 bits: the 128th lies at 0.99 of 2^32 bytes, the 129th at 2^32, which the
+    kernel that counts by tiles takes; K and V in the same memory."""
+    step = 1 << 24                                           # elements between two states
+    mem = torch.empty((n_k - 1) * step + 256, dtype=B, device=DEV)
+    k, v = (mem[at:].as_strided((1, 1, n_k, 128), (0, 0, step, 1)) for at in (0, 128))
+    g = torch.Generator(device=DEV).manual_seed(22)
+    k.copy_(torch.randn(1, 1, n_k, 128, generator=g, device=DEV))
+    v.copy_(torch.randn(1, 1, n_k, 128, generator=g, device=DEV))
+    mask = (torch.rand(1, n_k, generator=g, device=DEV) < 0.6).to(torch.uint8)
+    mask[0, -1] = 1
+    for T in (3, 70, 40000):
+        q = torch.randn(1, 1, T, 128, generator=g, device=DEV).to(B)
+        o, lse = torch.empty_like(q), torch.empty(1, 1, T, device=DEV)
+        forward(q, k, v, None, mask, o, lse)
+        r = ref.Cross(q, k.contiguous(), v.contiguous(), 128 ** -0.5, None, mask)
+        assert ref.worst(o, r.o, r.o_tol) <= 1 and ref.worst(lse, r.lse, r.lse_tol) <= 1
