@@ -1027,7 +1027,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) cross_grad_few_kernel(CrossGra
         s = over_row<LPK>(s);
         dp = over_row<LPK>(dp);
         const float p = on[u] ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -lse[r])) : 0.0f;
-        const float ds = p * (dp - delta[r]) * a.scale;
+        const float ds = on[u] ? p * (dp - delta[r]) * a.scale : 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           dq[r][e] = __builtin_fmaf(ds, kf[e], dq[r][e]);
@@ -1039,8 +1039,8 @@ __global__ void __launch_bounds__(64 * kFewWaves) cross_grad_few_kernel(CrossGra
       if (k < a.Nk) {
         const u32x4 x = {pack2<E>(dk[0], dk[1]), pack2<E>(dk[2], dk[3]), pack2<E>(dk[4], dk[5]), pack2<E>(dk[6], dk[7])};
         const u32x4 y = {pack2<E>(dv[0], dv[1]), pack2<E>(dv[2], dv[3]), pack2<E>(dv[4], dv[5]), pack2<E>(dv[6], dv[7])};
-        *reinterpret_cast<u32x4*>(dkb + k * a.dks[2]) = x;
-        *reinterpret_cast<u32x4*>(dvb + k * a.dvs[2]) = y;
+        *reinterpret_cast<u32x4*>(dkb + k * a.dks[2]) = on[u] ? x : zero;     // (0 times a row that holds NaN is none)
+        *reinterpret_cast<u32x4*>(dvb + k * a.dvs[2]) = on[u] ? y : zero;
       }
     }
   }
