@@ -851,12 +851,16 @@ CrossShape cross_shape(const pbsa_cross& p, bool masked) {
 }
 
 template <typename E, int D>
-void launch_typed(const CrossShape& s, const CrossArgs& a, int n, hipStream_t stream) {
+hipError_t launch_typed(const CrossShape& s, const CrossArgs& a, int n, hipStream_t stream) {
   const dim3 grid((unsigned)((s.units * s.parts + 7) / 8 * 8));
   if (s.by == By::rows) {
-    if (a.list) launch_attended(a.k_len, a.k_mask, a.mask_stride_b, n, a.Nk, const_cast<int32_t*>(a.list), const_cast<int32_t*>(a.counts), stream);
+    if (a.list) {
+      // without its list the next launch has nothing to go by
+      const hipError_t e = launch_attended(a.k_len, a.k_mask, a.mask_stride_b, n, a.Nk, const_cast<int32_t*>(a.list), const_cast<int32_t*>(a.counts), stream);
+      if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL((cross_rows_kernel<E, D>), grid, dim3(kThreads), 0, stream, a);
-    return;
+    return hipGetLastError();
   }
   const dim3 block(64 * s.waves);
   if (s.by == By::keys) hipLaunchKernelGGL((cross_keys_kernel<E, D>), grid, block, 0, stream, a);
@@ -864,6 +868,7 @@ void launch_typed(const CrossShape& s, const CrossArgs& a, int n, hipStream_t st
   else if (a.M == 2) hipLaunchKernelGGL((cross_few_kernel<E, D, 2>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((cross_few_kernel<E, D, 4>), grid, block, 0, stream, a);
   if (s.parts > 1) hipLaunchKernelGGL((cross_join_kernel<E, D>), dim3((unsigned)(s.units * s.part_rows)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -909,14 +914,8 @@ hipError_t launch_cross(const pbsa_cross& p, const void* Q, const void* K, const
   a.part_o = static_cast<float*>(ws);
   a.part_rows = s.part_rows;
   a.part_ml = a.part_o + (size_t)(s.units * s.parts) * s.part_rows * p.d;
-  if (p.dtype == PBSA_BF16) {
-    if (p.d == 64) launch_typed<__bf16, 64>(s, a, p.n, stream);
-    else launch_typed<__bf16, 128>(s, a, p.n, stream);
-  } else {
-    if (p.d == 64) launch_typed<_Float16, 64>(s, a, p.n, stream);
-    else launch_typed<_Float16, 128>(s, a, p.n, stream);
-  }
-  return hipGetLastError();
+  if (p.dtype == PBSA_BF16) return p.d == 64 ? launch_typed<__bf16, 64>(s, a, p.n, stream) : launch_typed<__bf16, 128>(s, a, p.n, stream);
+  return p.d == 64 ? launch_typed<_Float16, 64>(s, a, p.n, stream) : launch_typed<_Float16, 128>(s, a, p.n, stream);
 }
 
 }  // namespace pbsa

@@ -1127,7 +1127,7 @@ CrossGradShape cross_grad_shape(const pbsa_cross& p) {
 }
 
 template <typename E, int D>
-void launch_typed(const CrossGradShape& s, const CrossGradArgs& a, int n, hipStream_t stream) {
+hipError_t launch_typed(const CrossGradShape& s, const CrossGradArgs& a, int n, hipStream_t stream) {
   const auto grid = [](int64_t k) { return dim3((unsigned)((k + 7) / 8 * 8)); };
   if (s.waves > 0) {
     const dim3 at = grid((int64_t)a.row_units * a.key_parts), block(64 * s.waves);
@@ -1136,14 +1136,18 @@ void launch_typed(const CrossGradShape& s, const CrossGradArgs& a, int n, hipStr
     else hipLaunchKernelGGL((cross_grad_few_kernel<E, D, 4>), at, block, 0, stream, a);
     if (a.key_parts > 1)
       hipLaunchKernelGGL((cross_grad_few_join_kernel<E, D>), dim3((unsigned)(a.row_units * a.M)), dim3(kThreads), 0, stream, a);
-    return;
+    return hipGetLastError();
   }
-  if (a.list) launch_attended(a.k_len, a.k_mask, a.mask_stride_b, n, a.Nk, const_cast<int32_t*>(a.list), const_cast<int32_t*>(a.counts), stream);
+  if (a.list) {
+    // without its list the next launch has nothing to go by
+    const hipError_t e = launch_attended(a.k_len, a.k_mask, a.mask_stride_b, n, a.Nk, const_cast<int32_t*>(a.list), const_cast<int32_t*>(a.counts), stream);
+    if (e != hipSuccess) return e;
+  }
   if (s.small) {
     hipLaunchKernelGGL((cross_grad_small_kernel<E, D>), grid((int64_t)a.row_units * a.key_parts + a.key_units), dim3(kThreads), 0, stream, a);
     if (a.key_parts > 1)
       hipLaunchKernelGGL((cross_dq_join_kernel<E, D>), dim3((unsigned)(a.row_units * (D / 8))), dim3(kThreads), 0, stream, a);
-    return;
+    return hipGetLastError();
   }
   if (a.row_units > 0) {
     hipLaunchKernelGGL((cross_dq_kernel<E, D>), grid((int64_t)a.row_units * a.key_parts), dim3(kThreads), 0, stream, a);
@@ -1155,6 +1159,7 @@ void launch_typed(const CrossGradShape& s, const CrossGradArgs& a, int n, hipStr
     if (a.parts > 1)
       hipLaunchKernelGGL((cross_dkv_join_kernel<E, D>), dim3((unsigned)(a.key_units * 2 * (D / 8))), dim3(kThreads), 0, stream, a);
   }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -1219,14 +1224,8 @@ hipError_t launch_cross_bwd(const pbsa_cross& p, const void* Q, const void* K, c
   }
   a.part_q = reinterpret_cast<float*>(take(s.part_q_bytes));
   a.part = reinterpret_cast<float*>(at);
-  if (p.dtype == PBSA_BF16) {
-    if (p.d == 64) launch_typed<__bf16, 64>(s, a, p.n, stream);
-    else launch_typed<__bf16, 128>(s, a, p.n, stream);
-  } else {
-    if (p.d == 64) launch_typed<_Float16, 64>(s, a, p.n, stream);
-    else launch_typed<_Float16, 128>(s, a, p.n, stream);
-  }
-  return hipGetLastError();
+  if (p.dtype == PBSA_BF16) return p.d == 64 ? launch_typed<__bf16, 64>(s, a, p.n, stream) : launch_typed<__bf16, 128>(s, a, p.n, stream);
+  return p.d == 64 ? launch_typed<_Float16, 64>(s, a, p.n, stream) : launch_typed<_Float16, 128>(s, a, p.n, stream);
 }
 
 }  // namespace pbsa

@@ -10,10 +10,10 @@ namespace {
 
 constexpr int kThreads = 1024, kEach = 16;
 
-__global__ void __launch_bounds__(kThreads) attended_kernel(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int Nk,
-                                                            int32_t* list, int32_t* counts) {
-  __shared__ int wave_sum[kThreads / 64];
-  const int64_t b = blockIdx.x;
+constexpr int kMostGroups = 1 << 21;
+
+__device__ void list_sequence(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int Nk, int32_t* list, int32_t* counts,
+                              int64_t b, int* wave_sum) {
   const uint8_t* const mask = k_mask + b * mask_stride_b;
   int32_t* const to = list + b * Nk;
   const int len = k_len ? min(max(k_len[b], 0), Nk) : Nk;
@@ -49,12 +49,19 @@ __global__ void __launch_bounds__(kThreads) attended_kernel(const int32_t* k_len
   }
   if (threadIdx.x == 0) counts[b] = before;
 }
+__global__ void __launch_bounds__(kThreads) attended_kernel(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int n, int Nk,
+                                                            int32_t* list, int32_t* counts) {
+  __shared__ int wave_sum[kThreads / 64];
+  for (int64_t b = blockIdx.x; b < n; b += gridDim.x) list_sequence(k_len, k_mask, mask_stride_b, Nk, list, counts, b, wave_sum);
+}
 
 }  // namespace
 
-void launch_attended(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int n, int Nk, int32_t* list, int32_t* counts,
-                     hipStream_t stream) {
-  hipLaunchKernelGGL(attended_kernel, dim3((unsigned)n), dim3(kThreads), 0, stream, k_len, k_mask, mask_stride_b, Nk, list, counts);
+hipError_t launch_attended(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int n, int Nk, int32_t* list, int32_t* counts,
+                           hipStream_t stream) {
+  hipLaunchKernelGGL(attended_kernel, dim3((unsigned)(n < kMostGroups ? n : kMostGroups)), dim3(kThreads), 0, stream, k_len, k_mask, mask_stride_b,
+                     n, Nk, list, counts);
+  return hipGetLastError();
 }
 
 }  // namespace pbsa

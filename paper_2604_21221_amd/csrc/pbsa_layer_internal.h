@@ -33,8 +33,8 @@ size_t cross_workspace_bytes(const pbsa_cross& p, bool masked);
 // the list [n][Nk] behind them (pbsa_cross_list.hip).
 inline size_t attended_first(int n) { return ((size_t)n + 63) & ~(size_t)63; }
 inline size_t attended_bytes(int n, int Nk) { return (attended_first(n) + (size_t)n * Nk) * sizeof(int32_t); }
-void launch_attended(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int n, int Nk, int32_t* list, int32_t* counts,
-                     hipStream_t stream);
+hipError_t launch_attended(const int32_t* k_len, const uint8_t* k_mask, int64_t mask_stride_b, int n, int Nk, int32_t* list, int32_t* counts,
+                           hipStream_t stream);
 hipError_t launch_cross(const pbsa_cross& p, const void* Q, const void* K, const void* V, const int32_t* k_len, const uint8_t* k_mask,
                         void* O, float* lse, void* ws, hipStream_t stream);
 size_t cross_bwd_workspace_bytes(const pbsa_cross& p);
