@@ -14,6 +14,8 @@
 // Measured, at 21504 x 12 x 128 of two tensors, 265 MB: 53 us, 5.0 TB/s (a copy of 1 GiB: 5.15).  At 4680 x 12 x 128 with the norm,
 // 58 MB: 13.0 us; its backward, 86 MB: 20.6 us and 4.5 for the sum of the workgroups' shares of the weights' gradients: there
 // a third of the time is launch and first loads, and the backward's 350 instructions for a row of a lane are another.
+#include <algorithm>
+
 #include "pbsa_layer_internal.h"
 
 namespace pbsa {
@@ -22,6 +24,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTok = 16;          // tokens of a workgroup
 constexpr int kMaxGroups = 1024;     // workgroups of a backward launch for a tensor, each of which leaves one partial sum per weight
+constexpr int kMostGroups = 1 << 23; // of a forward launch, which holds fewer than 2^32 threads in a dimension
 
 struct RotaryArgs {
   int T, H[2], d, rot, n_axes, pairs0, pairs01;
@@ -183,9 +186,9 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
 
   for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
     const int64_t b = g / a.groups_t;
-    const int t0 = (int)(g - b * a.groups_t) << a.tok_log, t = t0 + tk;
-    const bool on_t = own_c && t < a.T;
-    const int64_t tt = min(t, a.T - 1);
+    const int t0 = (int)(g - b * a.groups_t) << a.tok_log, last = a.T - 1 - t0;   // the group's last token, from its first
+    const bool on_t = own_c && tk <= last;
+    const int64_t tt = t0 + min(tk, last);
     const E* x = x0 + b * a.xs[i][0] + tt * a.xs[i][2] + h0 * a.xs[i][1];
     const E* dy = kGrad ? dy0 + b * a.dys[i][0] + tt * a.dys[i][2] + h0 * a.dys[i][1] : nullptr;
     E* y = y0 + b * a.ys[i][0] + tt * a.ys[i][2] + h0 * a.ys[i][1];
@@ -213,11 +216,11 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
     };
     fetch(h0);
     // ---- cosines and sines of the workgroup's tokens ------------------------------------------------------------------
-    if (kGrad) __syncthreads();                    // the previous group's are read
+    if (kGrad || g != blockIdx.x) __syncthreads(); // the previous group's are read
     if (my_tok < tok) {
       const int64_t* const pos = a.pos + b * a.pos_stride_b + axis;
       for (int k = my_tok; k < tok; k += tok_step) {
-        const double at = (double)pos[(int64_t)min(t0 + k, a.T - 1) * a.n_axes];
+        const double at = (double)pos[(int64_t)(t0 + min(k, last)) * a.n_axes];
         const double turn = fma(at, f, -rint(at * f)) + at * f2;
         float s, co;
         sincospif((float)(2.0 * turn), &s, &co);
@@ -388,8 +391,9 @@ RotaryShape rotary_shape(const pbsa_rotary& p) {
   // As many tokens as leave a workgroup to each compute unit for each tensor: what a workgroup does once costs more than the
   // uneven end of a launch (4680 tokens x 12 x 128 of two tensors: 16 tokens 13.0 us, 8 13.8, 4 16.8, 32 16.7; backward 20.6,
   // 22.8, 28, 25.7; 1000 x 5 x 64 in binary32: 4 tokens 5.7, 1 7.5).
-  while (s.tok_log > 0 && (int64_t)p.n * ((p.T + (1 << s.tok_log) - 1) >> s.tok_log) < 256) --s.tok_log;
-  s.groups_t = (p.T + (1 << s.tok_log) - 1) >> s.tok_log;
+  const auto groups_t = [&] { return ((int64_t)p.T + (1 << s.tok_log) - 1) >> s.tok_log; };
+  while (s.tok_log > 0 && p.n * groups_t() < 256) --s.tok_log;
+  s.groups_t = (int)groups_t();
   s.groups = (int64_t)p.n * s.groups_t;
   return s;
 }
@@ -449,7 +453,7 @@ hipError_t launch_rotary(const pbsa_rotary& p, RotaryOp op, const RotaryTensors&
   a.freq = t.freq;
   a.part = static_cast<float*>(ws);
   const bool grad = op == RotaryOp::norm_grad;
-  const unsigned grid = p.Hq + p.Hk == 0 ? 0 : grad ? (unsigned)grad_groups(s) : (unsigned)s.groups;
+  const unsigned grid = p.Hq + p.Hk == 0 ? 0 : grad ? (unsigned)grad_groups(s) : (unsigned)std::min<int64_t>(s.groups, kMostGroups);
   if (grid > 0) {
     if (p.dtype == PBSA_BF16) launch_op<__bf16>(p, op, a, grid, stream);
     else if (p.dtype == PBSA_FP16) launch_op<_Float16>(p, op, a, grid, stream);
