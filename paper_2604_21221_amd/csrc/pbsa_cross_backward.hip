@@ -44,7 +44,7 @@ struct CrossGradArgs {
   const void* dO;
   const int32_t* k_len;
   const uint8_t* k_mask;
-  const int32_t* list;               // [n][Nk] attended states and [n] their number, or nullptr: no mask (dQ)
+  const int32_t* list;               // [n][Nk] attended states and [n] their number, or nullptr: no mask, or up to four rows
   const int32_t* counts;
   const float* lse;
   void* dQ;
@@ -122,20 +122,44 @@ __device__ __forceinline__ s16x8 operand_of(const uint32_t* p) {
 }
 
 // delta = sum P dP is rowsum(dO O), but O has been rounded.  Where a row has many states O is small beside V and that is lost in
-// the rounding of dS; where it has a few, dP - delta can be a small difference of larger numbers.  So with up to kFewStates the
-// sum itself is formed, in binary32.  Error of dQ and dK in bf16, of their norm, with two states 0.0050 by the outputs, 0.0023
+// the rounding of dS; where it has a few, dP - delta can be a small difference of larger numbers.  So where a sequence attends up to
+// kFewStates, however many it has room for, the sum itself is formed, in binary32.  Error of dQ and dK in bf16, of their norm, with two states 0.0050 by the outputs, 0.0023
 // by the sum; eight 0.0033 and 0.0024; sixteen 0.0030 and 0.0024.  Time with three, 5 x 8676 rows of 15 heads of 64: 167 us and
 // 187; with ten, 5 x 316 of 14 of 128: 26 and 37.
 constexpr int kFewStates = 8;
-// Of R rows, each over D / 8 lanes, 8 elements a lane; lse in powers of two
+// Those of a mask, in order, by a wave: their number if there are up to kFewStates, else more than that.  Whole waves of a workgroup
+// may do so with the same `few` in LDS: they write the same.  Mostly the first 64 states tell; else 1024 to a turn, bound by latency.
+__device__ __forceinline__ int few_attended(const Attended& keys, int lane, int* few) {
+  constexpr int kLook = 16;
+  int count = __popcll(keys.bits<64>(0, lane));
+  if (__builtin_expect(count <= kFewStates, 0)) {
+    count = 0;
+    for (int k0 = 0; k0 < keys.len && count <= kFewStates; k0 += 64 * kLook) {
+      uint64_t bits[kLook];
+      int more = 0;
+#pragma unroll
+      for (int u = 0; u < kLook; ++u) {
+        bits[u] = keys.bits<64>(k0 + 64 * u, lane);
+        more += __popcll(bits[u]);
+      }
+      if (count + more > kFewStates) return count + more;
+#pragma unroll
+      for (int u = 0; u < kLook; ++u)
+        for (uint64_t m = bits[u]; m != 0; m &= m - 1) few[count++] = k0 + 64 * u + __builtin_ctzll(m);
+    }
+  }
+  return count;
+}
+// Of R rows, each over D / 8 lanes, 8 elements a lane; lse in powers of two; the n attended states are the first ones, or those of a
+// list
 template <typename E, int D, int R>
-__device__ __forceinline__ void sum_delta(const CrossGradArgs& a, const Attended& keys, int64_t b, int hk, int d0, const float (&q)[R][8],
+__device__ __forceinline__ void sum_delta(const CrossGradArgs& a, const int32_t* list, int n, int64_t b, int hk, int d0, const float (&q)[R][8],
                                           const float (&g)[R][8], const float (&lse)[R], float (&delta)[R]) {
   typedef typename Vec<E>::x8 x8;
 #pragma unroll
   for (int r = 0; r < R; ++r) delta[r] = 0.0f;
-  for (int j = 0; j < keys.len; ++j) {
-    if (keys.mask && keys.mask[j] == 0) continue;
+  for (int i = 0; i < n; ++i) {
+    const int j = list ? list[i] : i;
     const x8 k = *reinterpret_cast<const x8*>(reinterpret_cast<const E*>(a.K) + b * a.ks[0] + hk * a.ks[1] + j * a.ks[2] + d0);
     const x8 v = *reinterpret_cast<const x8*>(reinterpret_cast<const E*>(a.V) + b * a.vs[0] + hk * a.vs[1] + j * a.vs[2] + d0);
 #pragma unroll
@@ -348,12 +372,11 @@ __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* r
   const int mm = min(m, a.M - 1), t = a.G == 1 ? mm : mm / a.G, h = hk * a.G + (mm - t * a.G);
   const float lse = a.lse[(b * a.Hk * a.G + h) * a.T + t];
   w.lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
-  if (a.Nk <= kFewStates) {          // (sum_delta; here a lane has half of its row)
+  if (states.count <= kFewStates) {  // (sum_delta; here a lane has half of its row)
     typedef typename Vec<E>::x8 x8;
-    const Attended keys = attended_of(a.k_len, a.k_mask, a.mask_stride_b, b, a.Nk);
     w.delta = 0.0f;
-    for (int j = 0; j < keys.len; ++j) {
-      if (keys.mask && keys.mask[j] == 0) continue;
+    for (int i = 0; i < states.count; ++i) {
+      const int j = states.list ? states.list[i] : i;
       const char* const kp = states.kb + j * states.ks + 16 * half;
       const char* const vp = states.vb + j * states.vs + 16 * half;
       float s = 0.0f, dp = 0.0f;
@@ -692,6 +715,8 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
 
   const Attended keys = attended_of(a.k_len, a.k_mask, a.mask_stride_b, b, a.Nk);
   const int m_end = min(a.M, (part + 1) * a.part_rows), len = keys.len;
+  const int32_t* const list = OWN && a.list ? a.list + b * a.Nk : nullptr;
+  const int count = OWN && a.list ? __builtin_amdgcn_readfirstlane(a.counts[b]) : len;   // of attended states
   const bool on = (keys.bits<32>(key0, lane) >> (lane & 31)) & 1;
   // a tile past the sequence's states has nothing to add up
   const int m_first = (unit - bh * a.key_tiles) * 128 >= len ? m_end : min(part * a.part_rows, m_end);
@@ -761,7 +786,7 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
           delta[u] = over_row<T::CH>(delta[u]);
           lse[u] = lse[u] == -INFINITY ? INFINITY : lse[u] * kLog2e;
         }
-        if (a.Nk <= kFewStates) {
+        if (count <= kFewStates) {
           float qf[kBatch][8], gf[kBatch][8];
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
@@ -772,7 +797,7 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
               gf[u][e] = (float)x[u][e];
             }
           }
-          sum_delta<E, D, kBatch>(a, keys, b, hk, lane % T::CH * 8, qf, gf, lse, delta);
+          sum_delta<E, D, kBatch>(a, list, count, b, hk, lane % T::CH * 8, qf, gf, lse, delta);
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
@@ -955,6 +980,7 @@ template <typename E, int D, int MR>
 __global__ void __launch_bounds__(64 * kFewWaves) cross_grad_few_kernel(CrossGradArgs a) {
   constexpr int LPK = D / 8, KPI = 64 / LPK, kBatch = MR == 4 ? 2 : 4;
   __shared__ float sums[kFewWaves][MR][D];
+  __shared__ int few[kFewStates];    // the attended states of a mask, if they are so few
   typedef typename Vec<E>::x8 x8;
   const int unit_part = place(blockIdx.x, a.row_units * a.key_parts);
   if (unit_part < 0) return;
@@ -983,11 +1009,12 @@ __global__ void __launch_bounds__(64 * kFewWaves) cross_grad_few_kernel(CrossGra
   const Attended keys = attended_of(a.k_len, a.k_mask, a.mask_stride_b, b, a.Nk);
   const int len = keys.len;
   const uint8_t* const mask = keys.mask;
-  if (a.Nk <= kFewStates) sum_delta<E, D, MR>(a, keys, b, hk, d0, q, g, lse, delta);
   const E* const kb = reinterpret_cast<const E*>(a.K) + b * a.ks[0] + hk * a.ks[1] + d0;
   const E* const vb = reinterpret_cast<const E*>(a.V) + b * a.vs[0] + hk * a.vs[1] + d0;
   E* const dkb = reinterpret_cast<E*>(a.dK) + b * a.dks[0] + hk * a.dks[1] + d0;
   E* const dvb = reinterpret_cast<E*>(a.dV) + b * a.dvs[0] + hk * a.dvs[1] + d0;
+  const int count = mask ? few_attended(keys, lane, few) : len;
+  if (count <= kFewStates) sum_delta<E, D, MR>(a, mask ? few : nullptr, count, b, hk, d0, q, g, lse, delta);
   for (int64_t k0 = (int64_t)(part * waves + wave) * KPI * kBatch; k0 < a.Nk; k0 += (int64_t)a.key_parts * waves * KPI * kBatch) {
     u32x4 kr[kBatch], vr[kBatch];
     bool on[kBatch];
