@@ -100,7 +100,8 @@ int pbsa_cross_attention_fwd(const pbsa_cross* p, const void* Q, const void* K, 
                              const uint8_t* k_mask, void* O, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Gradients of the forward call from its inputs, its O and lse, and dO.  dQ, dK and dV are written in full, in .dtype; dK and
- * dV are the sums over the query heads that share a head. */
+ * dV are the sums over the query heads that share a head.  In fp16 the gradients of the scores are scaled into the type's range by
+ * the rows' largest |dO|; with values that pass it even so (a sum of |V| over d of more than 2^17) the call is right and slow. */
 int pbsa_cross_bwd_workspace_bytes(const pbsa_cross* p, size_t* out);
 int pbsa_cross_attention_bwd(const pbsa_cross* p, const void* Q, const void* K, const void* V, const int32_t* k_len,
                              const uint8_t* k_mask, const void* O, const void* dO, const float* lse, void* dQ, void* dK, void* dV,

@@ -65,7 +65,9 @@ __device__ __forceinline__ int place(int bx, int n) {
 }
 
 // k of 2^-k for gradients of at most `top`, which are below 1 by it: |dS| = P |dP - sum P dP| is at most P (1 - P) times how far
-// two of dO V^T lie apart, half the sum of |V| over d, and fp16 holds it as long as that sum is below 2^17.
+// two of dO V^T lie apart, half the sum of |V| over d, and fp16 holds it as long as that sum is below 2^17.  Where it does not, the
+// wave forms its sums again in binary32 (dq_plain, dk_plain): without matrix instructions, a matter of being right (4680 x 512 x 12 of
+// 128 with every wave doing so: 5.4 ms).
 __device__ __forceinline__ float lift(float top) {
   if (!(top > 0.0f) || !(top < INFINITY)) return 0.0f;
   return fminf(fmaxf((float)__builtin_amdgcn_frexp_expf(top), -60.0f), 60.0f);
@@ -101,6 +103,8 @@ __device__ __forceinline__ float over_row(float v) {
   return v;
 }
 
+// Whether dS of a wave's has been infinite in a column that counts: then all of the column's sums are infinite or NaN, and one tells.
+__device__ __forceinline__ bool beyond(float sum, bool counts) { return __any(counts && !(fabsf(sum) < INFINITY)); }
 template <typename E>
 __device__ __forceinline__ void store4(E* to, float x, float y, float z, float w) {
   const u32x2 v = {pack2<E>(x, y), pack2<E>(z, w)};
@@ -306,6 +310,52 @@ __device__ __forceinline__ char* row_piece(const CrossGradArgs& a, const void* b
   return reinterpret_cast<char*>(const_cast<void*>(base)) + 2 * (b * st[0] + h * st[1] + t * st[2]) + c;
 }
 
+// dQ of a wave's 32 rows again where fp16 has not held their dS: in binary32, a row after the other, the states over groups of D / 8
+// lanes.  Written over what has been written.
+template <typename E, int D>
+__device__ __forceinline__ void dq_plain(const CrossGradArgs& a, const char* kb, const char* vb, const int32_t* list, int begin, int end, int64_t b,
+                                         int hk, int m0, float lse_of, float delta_of, f32x4* part) {
+  typedef typename Vec<E>::x8 x8;
+  constexpr int LPK = D / 8, KPI = 64 / LPK;
+  const int lane = threadIdx.x & 63, grp = lane / LPK, c = lane % LPK;
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+#pragma unroll 1
+  for (int r = 0; r < 32 && m0 + r < a.M; ++r) {
+    const float lse = __shfl(lse_of, r), delta = __shfl(delta_of, r);
+    const x8 q = *reinterpret_cast<const x8*>(row_piece<D>(a, a.Q, a.qs, b, hk, m0 + r, 16 * c));
+    const x8 g = *reinterpret_cast<const x8*>(row_piece<D>(a, a.dO, a.gs, b, hk, m0 + r, 16 * c));
+    float dq[8] = {};
+#pragma unroll 1
+    for (int i0 = begin; i0 < end; i0 += KPI) {
+      const int i = min(i0 + grp, end - 1);
+      const int64_t j = list ? list[i] : i;
+      const x8 k = *reinterpret_cast<const x8*>(kb + j * 2 * a.ks[2] + 16 * c), v = *reinterpret_cast<const x8*>(vb + j * 2 * a.vs[2] + 16 * c);
+      float s = 0.0f, dp = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s = __builtin_fmaf((float)k[e], (float)q[e], s);
+        dp = __builtin_fmaf((float)v[e], (float)g[e], dp);
+      }
+      s = over_row<LPK>(s);
+      dp = over_row<LPK>(dp);
+      const float ds = i0 + grp < end ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -lse)) * (dp - delta) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dq[e] = __builtin_fmaf(ds, (float)k[e], dq[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dq[e] = over_groups<LPK>(dq[e]) * a.scale;
+    if (grp != 0) continue;
+    if (part) {
+      part[c * 64 + r] = f32x4{dq[0], dq[1], dq[2], dq[3]};
+      part[c * 64 + 32 + r] = f32x4{dq[4], dq[5], dq[6], dq[7]};
+    } else {
+      E* const to = reinterpret_cast<E*>(row_piece<D>(a, a.dQ, a.dqs, b, hk, m0 + r, 16 * c));
+      store4<E>(to, dq[0], dq[1], dq[2], dq[3]);
+      store4<E>(to + 4, dq[4], dq[5], dq[6], dq[7]);
+    }
+  }
+}
+
 // A workgroup's part of dQ; ring: kRowBytes of its LDS.  STATS: it leaves what the launch of dK and dV needs.
 template <typename E, int D, bool STATS>
 __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* ring, int unit_part) {
@@ -467,18 +517,25 @@ __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* r
 #pragma unroll
     for (int dt = 0; dt < T::DT; ++dt) settle(w.dq[dt]);
   }
+  const bool again = kLift && beyond(w.dq[0][0], on && top < INFINITY);
+  const auto plain = [&](f32x4* to) {
+    if constexpr (kLift)
+      if (__builtin_expect(again, 0))
+        dq_plain<E, D>(a, states.kb, states.vb, states.list, first * kKeys, min(states.count, (first + n_tiles) * kKeys), b, hk, m0, w.lse - k, w.delta, to);
+  };
   const float f = kLift ? a.scale * __builtin_amdgcn_exp2f(k) : a.scale;
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) w.dq[dt][v] *= f;
   if (a.key_parts > 1) {
-    f32x4* const to = reinterpret_cast<f32x4*>(a.part_q) + (((int64_t)part * a.row_units + unit) * kWaves + wave) * kSlots * 64 + lane;
+    f32x4* const to = reinterpret_cast<f32x4*>(a.part_q) + (((int64_t)part * a.row_units + unit) * kWaves + wave) * kSlots * 64;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const f32x16& x = w.dq[s / 4];
-      to[s * 64] = f32x4{x[4 * (s % 4)], x[4 * (s % 4) + 1], x[4 * (s % 4) + 2], x[4 * (s % 4) + 3]};
+      to[s * 64 + lane] = f32x4{x[4 * (s % 4)], x[4 * (s % 4) + 1], x[4 * (s % 4) + 2], x[4 * (s % 4) + 3]};
     }
+    plain(to);
     return;
   }
   // through LDS: whole rows to memory
@@ -499,6 +556,7 @@ __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* r
     const u32x4 v = *(lds_16_t)(uintptr_t)(out + j * 1024 + lane * 16);
     if (m0 + rr < a.M) *reinterpret_cast<u32x4*>(row_piece<D>(a, a.dQ, a.dqs, b, hk, m0 + rr, c)) = v;
   }
+  plain(nullptr);
 }
 template <int D>
 constexpr int kRowBytes = 5 * RowPipe<D>::kTile;                   // of LDS: three places of K, two of V
@@ -698,6 +756,53 @@ struct RowLoads {
   }
 };
 
+// dK of a wave's states again where fp16 has not held their dS: in binary32, a state after the other, the rows over groups of D / 8
+// lanes.  lse and delta: of the rows, tiles of 64 `step` apart.  Written over what has been written.
+template <typename E, int D>
+__device__ __forceinline__ void dk_plain(const CrossGradArgs& a, const float* lse, const float* delta, int step, int m_first, int m_end, int64_t b,
+                                         int hk, int key0, uint32_t on, f32x4* part) {
+  typedef typename Vec<E>::x8 x8;
+  constexpr int LPK = D / 8, KPI = 64 / LPK;
+  const int lane = threadIdx.x & 63, grp = lane / LPK, c = lane % LPK;
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+#pragma unroll 1
+  for (; on != 0; on &= on - 1) {
+    const int x = __builtin_ctz(on);
+    const int64_t key = key0 + x;
+    const x8 k = *reinterpret_cast<const x8*>(reinterpret_cast<const E*>(a.K) + b * a.ks[0] + hk * a.ks[1] + key * a.ks[2] + 8 * c);
+    const x8 v = *reinterpret_cast<const x8*>(reinterpret_cast<const E*>(a.V) + b * a.vs[0] + hk * a.vs[1] + key * a.vs[2] + 8 * c);
+    float dk[8] = {};
+#pragma unroll 1
+    for (int i0 = 0; i0 < m_end - m_first; i0 += KPI) {
+      const int i = min(i0 + grp, m_end - m_first - 1), at = i / 64 * step + i % 64;
+      const x8 q = *reinterpret_cast<const x8*>(row_piece<D>(a, a.Q, a.qs, b, hk, m_first + i, 16 * c));
+      const x8 g = *reinterpret_cast<const x8*>(row_piece<D>(a, a.dO, a.gs, b, hk, m_first + i, 16 * c));
+      float s = 0.0f, dp = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s = __builtin_fmaf((float)k[e], (float)q[e], s);
+        dp = __builtin_fmaf((float)v[e], (float)g[e], dp);
+      }
+      s = over_row<LPK>(s);
+      dp = over_row<LPK>(dp);
+      const float ds = i0 + grp < m_end - m_first ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -lse[at] - lift_p<E>())) * (dp - delta[at]) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dk[e] = __builtin_fmaf(ds, (float)q[e], dk[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dk[e] = over_groups<LPK>(dk[e]) * a.scale;
+    if (grp != 0) continue;
+    if (part) {
+      part[c * 64 + x] = f32x4{dk[0], dk[1], dk[2], dk[3]};
+      part[c * 64 + 32 + x] = f32x4{dk[4], dk[5], dk[6], dk[7]};
+    } else {
+      E* const to = reinterpret_cast<E*>(a.dK) + b * a.dks[0] + hk * a.dks[1] + key * a.dks[2] + 8 * c;
+      store4<E>(to, dk[0], dk[1], dk[2], dk[3]);
+      store4<E>(to + 4, dk[4], dk[5], dk[6], dk[7]);
+    }
+  }
+}
+
 // A workgroup's part of dK and dV; ring: kKeyBytes of its LDS.  OWN: up to three tiles of rows, whose lse and delta it forms by
 // itself; else they are those that the launch of dQ has left.
 template <typename E, int D, bool OWN>
@@ -717,7 +822,8 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
   const int m_end = min(a.M, (part + 1) * a.part_rows), len = keys.len;
   const int32_t* const list = OWN && a.list ? a.list + b * a.Nk : nullptr;
   const int count = OWN && a.list ? __builtin_amdgcn_readfirstlane(a.counts[b]) : len;   // of attended states
-  const bool on = (keys.bits<32>(key0, lane) >> (lane & 31)) & 1;
+  const uint32_t on_bits = (uint32_t)keys.bits<32>(key0, lane);
+  const bool on = on_bits >> (lane & 31) & 1;
   // a tile past the sequence's states has nothing to add up
   const int m_first = (unit - bh * a.key_tiles) * 128 >= len ? m_end : min(part * a.part_rows, m_end);
   const int n_tiles = (m_end - m_first + kRows - 1) / kRows;
@@ -726,9 +832,8 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
   for (int dt = 0; dt < T::DT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) w.dk[dt][v] = w.dv[dt][v] = 0.0f;
-  float unlift = a.scale;
+  float unlift = a.scale, top = 0.0f;                              // top: the largest |dO| of the rows
   if (n_tiles > 0) {
-    float top = 0.0f;                // the largest |dO| of the rows
     if constexpr (kLift && !OWN) {
       for (int i = m_first / 128 + lane; i * 128 < m_end; i += 64) top = fmaxf(top, a.top[(int64_t)bh * a.row_tiles + i]);
     }
@@ -902,6 +1007,17 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
       settle(w.dv[dt]);
     }
   }
+  const bool again = kLift && beyond(w.dk[0][0], on && top < INFINITY);
+  const auto plain = [&](f32x4* to) {
+    if constexpr (kLift) {
+      if (__builtin_expect(again, 0)) {
+        const int64_t row = (int64_t)bh * a.row_tiles * 128 + m_first;
+        const float* const own = reinterpret_cast<const float*>(ring + 3 * Z::kPlace);
+        dk_plain<E, D>(a, OWN ? own : a.stat_lse + row, OWN ? own + kRows : a.stat_delta + row, OWN ? 2 * kRows : kRows, m_first, m_end, b, hk, key0,
+                       on_bits, to);
+      }
+    }
+  };
   const float unlift_p = __builtin_amdgcn_exp2f(-lift_p<E>());
 #pragma unroll
   for (int dt = 0; dt < T::DT; ++dt) {
@@ -912,24 +1028,27 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
     }
   }
   if (a.parts > 1) {
-    f32x4* const to = reinterpret_cast<f32x4*>(a.part) + (((int64_t)part * a.key_units + unit) * 2 * kWaves + wave) * kSlots * 64 + lane;
+    f32x4* const to = reinterpret_cast<f32x4*>(a.part) + (((int64_t)part * a.key_units + unit) * 2 * kWaves + wave) * kSlots * 64;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const f32x16 &k = w.dk[s / 4], &v = w.dv[s / 4];
-      to[s * 64] = f32x4{k[4 * (s % 4)], k[4 * (s % 4) + 1], k[4 * (s % 4) + 2], k[4 * (s % 4) + 3]};
-      to[(kWaves * kSlots + s) * 64] = f32x4{v[4 * (s % 4)], v[4 * (s % 4) + 1], v[4 * (s % 4) + 2], v[4 * (s % 4) + 3]};
+      to[s * 64 + lane] = f32x4{k[4 * (s % 4)], k[4 * (s % 4) + 1], k[4 * (s % 4) + 2], k[4 * (s % 4) + 3]};
+      to[(kWaves * kSlots + s) * 64 + lane] = f32x4{v[4 * (s % 4)], v[4 * (s % 4) + 1], v[4 * (s % 4) + 2], v[4 * (s % 4) + 3]};
     }
+    plain(to);
     return;
   }
-  if (key >= a.Nk) return;
-  E* const tk = reinterpret_cast<E*>(a.dK) + b * a.dks[0] + hk * a.dks[1] + key * a.dks[2] + 4 * half;
-  E* const tv = reinterpret_cast<E*>(a.dV) + b * a.dvs[0] + hk * a.dvs[1] + key * a.dvs[2] + 4 * half;
+  if (key < a.Nk) {
+    E* const tk = reinterpret_cast<E*>(a.dK) + b * a.dks[0] + hk * a.dks[1] + key * a.dks[2] + 4 * half;
+    E* const tv = reinterpret_cast<E*>(a.dV) + b * a.dvs[0] + hk * a.dvs[1] + key * a.dvs[2] + 4 * half;
 #pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    const f32x16 &k = w.dk[s / 4], &v = w.dv[s / 4];
-    store4<E>(tk + 8 * s, k[4 * (s % 4)], k[4 * (s % 4) + 1], k[4 * (s % 4) + 2], k[4 * (s % 4) + 3]);
-    store4<E>(tv + 8 * s, v[4 * (s % 4)], v[4 * (s % 4) + 1], v[4 * (s % 4) + 2], v[4 * (s % 4) + 3]);
+    for (int s = 0; s < kSlots; ++s) {
+      const f32x16 &k = w.dk[s / 4], &v = w.dv[s / 4];
+      store4<E>(tk + 8 * s, k[4 * (s % 4)], k[4 * (s % 4) + 1], k[4 * (s % 4) + 2], k[4 * (s % 4) + 3]);
+      store4<E>(tv + 8 * s, v[4 * (s % 4)], v[4 * (s % 4) + 1], v[4 * (s % 4) + 2], v[4 * (s % 4) + 3]);
+    }
   }
+  plain(nullptr);
 }
 template <int D>
 constexpr int kKeyBytes = 3 * (KeyPipe<D>::kPlace + kStatPlace) + 16;        // of LDS: three places of Q and dO, of the rows' scalars
