@@ -68,9 +68,11 @@ __device__ __forceinline__ void clear(Softmax<D>& w) {
   w.mc = 0.0f;
 }
 
-// 32 states in LDS, where the lane reads K by rows and V by columns, of which those in `bits` are attended
-template <typename E, int D>
-__device__ __forceinline__ void attend(Softmax<D>& w, const s16x8 (&q)[D / 16], uint32_t k_at, uint32_t v_at, uint32_t bits, float c2, int half) {
+// 32 states in LDS, where the lane reads K by rows and V by columns, of which those in `bits` are attended; blank() is done where
+// those are not all, before V is read
+template <typename E, int D, typename Blank>
+__device__ __forceinline__ void attend(Softmax<D>& w, const s16x8 (&q)[D / 16], uint32_t k_at, uint32_t v_at, uint32_t bits, float c2, int half,
+                                       Blank blank) {
   using T = Tile<D>;
   f32x16 s;
 #pragma unroll
@@ -78,6 +80,7 @@ __device__ __forceinline__ void attend(Softmax<D>& w, const s16x8 (&q)[D / 16], 
 #pragma unroll
   for (int ks = 0; ks < T::KS; ++ks) s = mfma<E>(read_row(k_at ^ (ks << 5)), q[ks], s);
   if (bits != 0xFFFFFFFFu) {
+    blank();
     const uint32_t on = bits >> (4 * half);
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = (on >> row_of(v)) & 1 ? s[v] : -INFINITY;
@@ -216,7 +219,7 @@ __device__ __forceinline__ void put_pair(Probs& x, int v) {
 
 // Step A (of the even half tile) walks the second half of a tile's K and of the V before it and ends with the turn to the next
 // places: some slots before its end its own reads are back, what lies in LDS is passed on, and the reads of step B begin.
-// Step B walks first halves; extra(slot) issues the tile loads.
+// extra(slot) is what a wave does to its own loads then; in step B, which walks first halves, it issues the tile loads.
 template <typename E, int D, bool A, int R, typename Extra>
 __device__ __forceinline__ void slots(Group<D>& w, Pipe<D>& z, float c2, Extra& extra) {
   using T = Tile<D>;
@@ -235,6 +238,7 @@ __device__ __forceinline__ void slots(Group<D>& w, Pipe<D>& z, float c2, Extra& 
     else if constexpr (!A) z.f[R % kAhead] = operand<D, R + kAhead - N, T::SUB, true>(z);
     if constexpr (A && R == kTurn) {
       wait_loads();
+      extra(R);
       barrier();
       preload<D, 0, false, 0, R % kAhead + 1>(z);                  // into the places of operands that have been used
     }
@@ -417,7 +421,13 @@ __global__ void __launch_bounds__(kThreads, 2) cross_rows_kernel(CrossArgs a) {
       });
     }
     mask(w.s[0], i * kKeys);
-    step<E, D, true>(w, z, a.c2, none);
+    // V of what stands in for states past the last one is zero: 0 times an infinity of the last one's would be NaN
+    step<E, D, true>(w, z, a.c2, [&](int) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (i * kKeys + (wave * N + j) * T::RPI + lane / T::CH >= count) *(lds_w_t)(uintptr_t)(own + at(i) + kTileBytes + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    });
     mask(w.s[1], i * kKeys + 32);
     step<E, D, false>(w, z, a.c2, none);                           // (its S^T is of no tile)
     const uint32_t last = lds + at(i) + kTileBytes + T::SUB + col_at<D>(lane);
@@ -556,7 +566,15 @@ __global__ void __launch_bounds__(kThreads, 1) cross_keys_kernel(CrossArgs a) {
       for (int ks = 0; ks < T::KS; ++ks) q[ks] = read_row((q_at + row0) ^ (ks << 5));
     } else {
       const uint32_t here = lds + (t & 1) * 2 * kTileBytes;
-      if (on != 0) attend<E, D>(w, q, here + row0, here + kTileBytes + col0, on, a.c2, half);
+      if (on != 0) {
+        attend<E, D>(w, q, here + row0, here + kTileBytes + col0, on, a.c2, half, [&] {
+          // V of what stands in is zero: 0 times an infinity of another state's would be NaN (LDS takes a wave's accesses in order)
+          typedef __attribute__((address_space(3))) u32x4* lds_w_t;
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (!(on >> (j * T::RPI + lane / T::CH) & 1)) *(lds_w_t)(uintptr_t)(here + kTileBytes + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        });
+      }
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");         // the tile has been read
     }
     on = on_next;

@@ -52,3 +52,22 @@ def test_masked_states_far_apart_in_memory(n_k):
         forward(q, k, v, None, mask, o, lse)
         r = ref.Cross(q, k.contiguous(), v.contiguous(), 128 ** -0.5, None, mask)
         assert ref.worst(o, r.o, r.o_tol) <= 1 and ref.worst(lse, r.lse, r.lse_tol) <= 1
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [3, 40, 2100])
+@pytest.mark.parametrize("Nk,lens,keep", [(90, None, None), (90, (90, 33), None), (130, None, 0.5), (200, (150, 1), 0.7), (64, None, None), (1, None, None)])
+def test_infinite_values_are_the_rows_results(Nk, lens, keep, T, d):
+    """An infinity in V of an attended state, the first or the last one too, is an infinity of the outputs in its place."""
+    case = (2, T, Nk, 16, 16, d, B, "token", lens, keep)
+    q, k, v, k_len, k_mask, _ = made(case, seed=7)
+    at = ref.attended(2, Nk, k_len, k_mask, DEV)
+    for b in range(2):
+        own = at[b].nonzero().flatten()
+        if len(own):
+            v[b, 3, own[-1], 9], v[b, 5, own[0], 10] = math.inf, -math.inf
+    o, lse = torch.empty_like(q), torch.empty(2, 16, T, device=DEV)
+    forward(q, k, v, k_len, k_mask, o, lse)
+    r = ref.Cross(q, k, v, d ** -0.5, k_len, k_mask)
+    assert int(torch.isinf(r.o).sum()) == 2 * T * int(at.any(1).sum())
+    assert ref.worst(o, r.o, r.o_tol) <= 1 and ref.worst(lse, r.lse, r.lse_tol) <= 1
