@@ -136,6 +136,7 @@ __device__ __forceinline__ Row row_at_m(const CrossArgs& a, int hk, int m) {
 // a probability passes kTop is the half tile's part done again with a new one (precision in floating point is relative;
 // kTop leaves fp16, whose range ends at 2^16, room to both sides).
 constexpr float kTop = 4096.0f;
+constexpr float kNone = -1e30f;      // the reference where the first half tile's scores are all -infinite: the next finite one resets it
 
 // c += a b in place, as an instruction of its own: the compiler does not copy c (as it did, for the rare rescaling's sake), and
 // does not see a matrix instruction (settle).
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 2) cross_rows_kernel(CrossArgs a) {
 #pragma unroll
     for (int v = 1; v < 16; ++v) m = fmaxf(m, w.s[0][v]);
     m = swap_max(m);
-    w.mc = m == -INFINITY ? 0.0f : m * a.c2;
+    w.mc = m == -INFINITY ? kNone : m * a.c2;
     const auto none = [](int) {};
     int i = 0;
     for (; i + 1 < n_tiles; ++i) {

@@ -71,3 +71,18 @@ def test_infinite_values_are_the_rows_results(Nk, lens, keep, T, d):
     r = ref.Cross(q, k, v, d ** -0.5, k_len, k_mask)
     assert int(torch.isinf(r.o).sum()) == 2 * T * int(at.any(1).sum())
     assert ref.worst(o, r.o, r.o_tol) <= 1 and ref.worst(lse, r.lse, r.lse_tol) <= 1
+
+
+@pytest.mark.parametrize("first", [30, 40, 64, 100])
+@pytest.mark.parametrize("T", [3, 40, 2100])
+@pytest.mark.parametrize("far", [0.0, 40.0])
+def test_scores_of_minus_infinity_count_for_nothing(T, first, far):
+    """Attended states whose keys are -infinite draw nothing from rows of positive queries, wherever the other scores lie."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    q, k, v = (torch.randn(1, 16, t, 64, generator=g, device=DEV) for t in (T, 200, 200))
+    q, k, v = (0.1 + q.abs()).to(B), (k / 8 - far).to(B), v.to(B)
+    k[:, :, :first] = -math.inf
+    o, lse = torch.empty_like(q), torch.empty(1, 16, T, device=DEV)
+    forward(q, k, v, None, None, o, lse)
+    r = ref.Cross(q, k[:, :, first:], v[:, :, first:], 0.125)
+    assert ref.worst(o, r.o, r.o_tol) <= 1 and ref.worst(lse, r.lse, r.lse_tol) <= 1
