@@ -67,7 +67,7 @@ def _build_host() -> str:
     from torch.utils import cpp_extension
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
-    cmd += [f"-I{p}" for p in [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]]
+    cmd += [f"-I{p}" for p in [os.path.join(ROOT, "include"), *cpp_extension.include_paths(), sysconfig.get_paths()["include"]]]
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd += [os.path.join(CSRC, "pbsa_host.cpp"), "-o", HOST_LIB, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
     subprocess.run(cmd, check=True)

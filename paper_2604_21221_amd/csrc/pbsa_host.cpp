@@ -7,6 +7,8 @@
 
 #include <cstdint>
 
+#include "pbsa_layer.h"
+
 namespace {
 
 constexpr int kMaxArgs = 26;   // of pbsa_attention_fwd_plan_split, the longest
@@ -128,6 +130,86 @@ PyObject* plain_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// What a call on a pbsa_rotary or pbsa_cross (layer.py) takes beside the tensors that its description was made of: an argument that
+// is a tensor has to be of the type that the library reads, with `inner` elements in a row for each of n sequences, `step` apart.
+// Another type would be read past its end or as other numbers.  Addresses and None pass.
+struct Side {
+  const char* name;
+  at::ScalarType type;
+  int64_t n, step, inner;
+};
+bool side_fits(const Side& want, const at::Tensor& t) {
+  const bool bytes = want.type == at::kByte && (t.scalar_type() == at::kBool || t.scalar_type() == at::kChar);
+  if (t.scalar_type() != want.type && !bytes) return false;
+  if (want.n <= 0 || want.inner <= 0) return true;                 // nothing of it is looked at
+  if (t.is_contiguous()) return (double)t.numel() >= (double)(want.n - 1) * (double)want.step + (double)want.inner;
+  // sequences in the first dimension, elsewhere in memory or all the same one
+  if (t.dim() < 1 || t.size(0) < want.n || (want.n > 1 && t.stride(0) != want.step)) return false;
+  const at::Tensor one = t.select(0, 0);
+  return one.is_contiguous() && one.numel() >= want.inner;
+}
+bool sides_fit(const Side* want, PyObject* const* args, Py_ssize_t n) {
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!THPVariable_Check(args[i]) || side_fits(want[i], THPVariable_Unpack(args[i]))) continue;
+    const at::Tensor& t = THPVariable_Unpack(args[i]);
+    PyErr_Format(PyExc_ValueError, "pbsa: %s: %s, %lld in a row for each of %lld, wanted, not %lld of %s%s", want[i].name,
+                 want[i].type == at::kByte ? "bytes" : c10::toString(want[i].type), (long long)want[i].inner, (long long)want[i].n,
+                 (long long)t.numel(), c10::toString(t.scalar_type()), t.is_contiguous() ? "" : ", with gaps");
+    return false;
+  }
+  return true;
+}
+PyObject* g_rotary = nullptr;       // the types of pbsa_rotary and pbsa_cross, set once
+PyObject* g_cross = nullptr;
+// The description that is the first of `want` arguments; the caller holds it for the length of the call.
+template <typename P>
+const P* described(PyObject* type, PyObject* const* args, Py_ssize_t n, Py_ssize_t want) {
+  if (n != want) {
+    PyErr_SetString(PyExc_TypeError, "pbsa: wrong number of arguments");
+    return nullptr;
+  }
+  if (!type || Py_TYPE(args[0]) != reinterpret_cast<PyTypeObject*>(type)) {
+    PyErr_Format(PyExc_TypeError, "pbsa: a %s is wanted, not a %s", type ? reinterpret_cast<PyTypeObject*>(type)->tp_name : "description",
+                 Py_TYPE(args[0])->tp_name);
+    return nullptr;
+  }
+  int64_t at = 0;
+  return bytes_of(args[0], at) == Take::yes ? reinterpret_cast<const P*>(at) : nullptr;
+}
+// rotary(pbsa_rotary, pos, freq, wq, wk, dwq, dwk) and cross(pbsa_cross, k_len, k_mask, lse) -> address of the description
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const pbsa_rotary* const p = described<pbsa_rotary>(g_rotary, args, n, 7);
+  if (!p) return nullptr;
+  const Side w{"norm weights", at::kFloat, 1, 0, p->d}, dw{"gradients of the norm weights", at::kFloat, 1, 0, p->d};
+  const Side want[6] = {{"pos", at::kLong, p->n, p->pos_stride_b, (int64_t)p->T * p->n_axes}, {"freq", at::kDouble, 1, 0, p->rot / 2}, w, w, dw, dw};
+  return sides_fit(want, args + 1, 6) ? PyLong_FromVoidPtr(const_cast<pbsa_rotary*>(p)) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+PyObject* cross(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const pbsa_cross* const p = described<pbsa_cross>(g_cross, args, n, 4);
+  if (!p) return nullptr;
+  const Side want[3] = {{"k_len", at::kInt, p->n, 1, 1}, {"k_mask", at::kByte, p->n, p->mask_stride_b, p->Nk},
+                        {"lse", at::kFloat, p->n, (int64_t)p->Hq * p->T, (int64_t)p->Hq * p->T}};
+  return sides_fit(want, args + 1, 3) ? PyLong_FromVoidPtr(const_cast<pbsa_cross*>(p)) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+// setup_layer(type of pbsa_rotary, type of pbsa_cross)
+PyObject* setup_layer(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
+    PyErr_SetString(PyExc_TypeError, "pbsa: setup_layer takes two types");
+    return nullptr;
+  }
+  PyObject** const to[2] = {&g_rotary, &g_cross};
+  for (int i = 0; i < 2; ++i) {
+    Py_INCREF(args[i]);
+    Py_XDECREF(*to[i]);
+    *to[i] = args[i];
+  }
+  Py_RETURN_NONE;
+}
+
 // setup(type of pbsa_params, type of pbsa_grid, ctypes.Array)
 PyObject* setup(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 3 || !PyType_Check(args[0]) || !PyType_Check(args[1]) || !PyType_Check(args[2])) {
@@ -150,6 +232,9 @@ constexpr PyCFunction fast(F f) {
 PyMethodDef methods[] = {
     {"invoke", fast(invoke), METH_FASTCALL, "invoke(function address, kinds, *arguments) -> int or NotImplemented"},
     {"plain_rows", fast(plain_rows), METH_FASTCALL, "plain_rows(Kl, Vl, H, Nq, d, watched, *tensors) -> bool"},
+    {"rotary", fast(rotary), METH_FASTCALL, "rotary(pbsa_rotary, pos, freq, wq, wk, dwq, dwk) -> address"},
+    {"cross", fast(cross), METH_FASTCALL, "cross(pbsa_cross, k_len, k_mask, lse) -> address"},
+    {"setup_layer", fast(setup_layer), METH_FASTCALL, "setup_layer(pbsa_rotary, pbsa_cross)"},
     {"setup", fast(setup), METH_FASTCALL, "setup(pbsa_params, pbsa_grid, ctypes.Array)"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pbsa_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,8 +1,13 @@
 """Binding of include/pbsa_layer.h: what a layer runs around its block-sparse attention.  Same names, same library and the same
 manner as pbsa.py: a description made once (make_rotary, make_cross), tensors passed through, no fallback.
 
-Tensors are [n, heads, tokens, d] views with a contiguous last dimension, of any memory order.  rotary_frequencies makes the
-frequencies that the rotation takes, scaled for long contexts or not.
+Tensors are [n, heads, tokens, d] views with a contiguous last dimension, of any memory order.  Positions (int64), frequencies
+(float64), norm weights and their gradients (float32), lengths (int32), masks (bytes) and lse (float32) are refused (ValueError) where
+they are of another type, too small or not laid out as the description says.  rotary_frequencies makes the frequencies that the
+rotation takes, scaled for long contexts or not.
+
+The calls write into tensors that they are given, and autograd records none of them: what is to have a gradient goes through a
+torch.autograd.Function whose backward makes the _bwd call (pbsa_rotate with inverse=True).
 """
 from __future__ import annotations
 
@@ -150,6 +155,30 @@ def _described(p, kind):
     return ctypes.addressof(p)
 
 
+def _native():
+    """The binding's native half takes the place of the two functions below."""
+    global _rotary, _cross
+    try:
+        from . import _pbsa_host
+    except ImportError as e:
+        raise ImportError("the binding's native half is missing: build it with `python -m paper_2604_21221_amd.build`") from e
+    _pbsa_host.setup_layer(pbsa_rotary, pbsa_cross)
+    _rotary, _cross = _pbsa_host.rotary, _pbsa_host.cross
+
+
+def _rotary(*args):
+    """_rotary(description, pos, freq, wq, wk, dwq, dwk): the address of the description, with the arguments that it does not describe
+    checked against it (csrc/pbsa_host.cpp)"""
+    _native()
+    return _rotary(*args)
+
+
+def _cross(*args):
+    """_cross(description, k_len, k_mask, lse), likewise"""
+    _native()
+    return _cross(*args)
+
+
 def _call(name, *args):
     rc = pbsa._invoke(*_F[name], *args)
     if rc is NotImplemented:                 # anything but plain tensors and integers: ctypes and _ptr take it or refuse it
@@ -164,11 +193,11 @@ def _size(name, p, kind):
 
 
 def pbsa_rotate(p, Q, K, pos, freq, Qo, Ko, inverse=False, stream=None):
-    _call("pbsa_rotate", _described(p, pbsa_rotary), Q, K, pos, freq, Qo, Ko, int(inverse), pbsa._stream(stream))
+    _call("pbsa_rotate", _rotary(p, pos, freq, None, None, None, None), Q, K, pos, freq, Qo, Ko, int(inverse), pbsa._stream(stream))
 
 
 def pbsa_norm_rotate_fwd(p, Q, K, wq, wk, pos, freq, Qo, Ko, stream=None):
-    _call("pbsa_norm_rotate_fwd", _described(p, pbsa_rotary), Q, K, wq, wk, pos, freq, Qo, Ko, pbsa._stream(stream))
+    _call("pbsa_norm_rotate_fwd", _rotary(p, pos, freq, wq, wk, None, None), Q, K, wq, wk, pos, freq, Qo, Ko, pbsa._stream(stream))
 
 
 def pbsa_norm_rotate_workspace_bytes(p: pbsa_rotary) -> int:
@@ -177,7 +206,7 @@ def pbsa_norm_rotate_workspace_bytes(p: pbsa_rotary) -> int:
 
 def pbsa_norm_rotate_bwd(p, Q, K, wq, wk, pos, freq, dQo, dKo, dQ, dK, dwq, dwk, ws, stream=None):
     w, wb = pbsa._ws(ws)
-    _call("pbsa_norm_rotate_bwd", _described(p, pbsa_rotary), Q, K, wq, wk, pos, freq, dQo, dKo, dQ, dK, dwq, dwk, w, wb,
+    _call("pbsa_norm_rotate_bwd", _rotary(p, pos, freq, wq, wk, dwq, dwk), Q, K, wq, wk, pos, freq, dQo, dKo, dQ, dK, dwq, dwk, w, wb,
           pbsa._stream(stream))
 
 
@@ -187,7 +216,7 @@ def pbsa_cross_workspace_bytes(p: pbsa_cross) -> int:
 
 def pbsa_cross_attention_fwd(p, Q, K, V, k_len, k_mask, O, lse=None, ws=None, stream=None):
     w, wb = pbsa._ws(ws)
-    _call("pbsa_cross_attention_fwd", _described(p, pbsa_cross), Q, K, V, k_len, k_mask, O, lse, w, wb, pbsa._stream(stream))
+    _call("pbsa_cross_attention_fwd", _cross(p, k_len, k_mask, lse), Q, K, V, k_len, k_mask, O, lse, w, wb, pbsa._stream(stream))
 
 
 def pbsa_cross_bwd_workspace_bytes(p: pbsa_cross) -> int:
@@ -196,5 +225,5 @@ def pbsa_cross_bwd_workspace_bytes(p: pbsa_cross) -> int:
 
 def pbsa_cross_attention_bwd(p, Q, K, V, k_len, k_mask, O, dO, lse, dQ, dK, dV, ws, stream=None):
     w, wb = pbsa._ws(ws)
-    _call("pbsa_cross_attention_bwd", _described(p, pbsa_cross), Q, K, V, k_len, k_mask, O, dO, lse, dQ, dK, dV, w, wb,
+    _call("pbsa_cross_attention_bwd", _cross(p, k_len, k_mask, lse), Q, K, V, k_len, k_mask, O, dO, lse, dQ, dK, dV, w, wb,
           pbsa._stream(stream))
