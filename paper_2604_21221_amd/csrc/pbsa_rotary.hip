@@ -121,8 +121,7 @@ template <typename E, bool HALF, RotaryOp OP>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
   constexpr bool kGrad = OP == RotaryOp::norm_grad, kNorm = OP != RotaryOp::rotate;
   constexpr int kRows = kGrad ? 1 : 2;           // rows on their way while as many are worked on (what registers leave room for)
-  // [token][pair] cosine and sine; behind them, for a backward pass, those of elements that do not turn
-  __shared__ __align__(16) float2 turns[kMaxTok * PBSA_ROTARY_MAX_D / 2 + 4];
+  __shared__ __align__(16) float2 turns[kMaxTok * PBSA_ROTARY_MAX_D / 2];      // [token][pair] cosine and sine
   __shared__ __align__(16) float weights[kGrad ? PBSA_ROTARY_MAX_D : 4];
   __shared__ float sums[kGrad ? kThreads / 64 : 1][kGrad ? 16 * 16 : 1];
   const int i = blockIdx.y;                                        // the tensor
@@ -164,7 +163,6 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
     wa[j] = wb[j] = 1.0f;
   }
   if constexpr (kGrad) {
-    if (tid < 4) turns[kMaxTok * PBSA_ROTARY_MAX_D / 2 + tid] = make_float2(1.0f, 0.0f);
     if (tid < a.d) weights[tid] = w ? w[tid] : 1.0f;
   } else if (w) {
 #pragma unroll
@@ -229,9 +227,8 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
     }
     __syncthreads();
     f8 cs, sn;
-    const float2* const none = kGrad ? turns + kMaxTok * PBSA_ROTARY_MAX_D / 2 : turns;
-    const float2* const ta = on_a ? turns + tk * n_pairs + pa : none;
-    const float2* const tb = on_b ? turns + tk * n_pairs + pb : none;
+    const float2* const ta = on_a ? turns + tk * n_pairs + pa : turns;
+    const float2* const tb = on_b ? turns + tk * n_pairs + pb : turns;
     auto my_turns = [&] {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -276,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
               wa[j] = weights[oa + j];
               wb[j] = weights[ob + j];
             }
-            turn<HALF>(gp, gq, cs, sn, true, true);
+            turn<HALF>(gp, gq, cs, sn, on_a, on_b);
             float dot = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {

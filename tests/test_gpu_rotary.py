@@ -297,3 +297,27 @@ def test_empty_gradients_are_zero():
     backward(p, q, q, (None, None), torch.empty(2, 0, 1, dtype=torch.int64, device=DEV), torch.empty(32, dtype=torch.float64, device=DEV),
              q, q, q, q, dw)
     assert (dw == 0).all()
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_an_infinite_gradient_reaches_its_own_weight_alone(half, dtype):
+    """An infinity in an element that is not rotated: its weight's gradient is infinite, the other ones are as they are, and of the
+    row's own gradient nothing is NaN but what the formula makes so."""
+    g = torch.Generator(device=DEV).manual_seed(9)
+    q, dy = (torch.randn(1, 2, 9, 64, generator=g, device=DEV).to(dtype) for _ in range(2))
+    q[0, 1, 3, 40] = 0.5
+    dy[0, 1, 3, 40] = math.inf
+    dq, dw = torch.empty_like(q), torch.empty(64, device=DEV)
+    freq, _ = layer.rotary_frequencies((16,), device=DEV)
+    pos = torch.arange(9, device=DEV).view(1, 9, 1) + 1
+    p = layer.make_rotary(q, None, dy, None, sections=(16,), half=half, dq=dq)
+    backward(p, q, None, (None, None), pos, freq, dy, None, dq, None, (dw, None))
+    gr = ref.rotate(dy.double(), ref.angles(pos, freq, (16,)), 32, half, 1.0, inverse=True)
+    want, want_w, _, size_w = ref.norm_grad(q.double(), None, gr, 1e-6)
+    assert torch.isinf(want_w).sum() == 1 and torch.isnan(want).sum() == 1
+    fine = torch.isfinite(want_w)
+    assert torch.equal(dw[~fine], want_w[~fine].float())
+    gm = torch.where(torch.isinf(gr), 0.0, ref.rotate(dy.double(), ref.angles(pos, freq, (16,)), 32, half, 1.0, inverse=True, magnitude=True))
+    assert ref.worst(dw[fine], want_w[fine], 160 * F * size_w(gm)[fine]) <= 1
+    assert torch.equal(torch.isnan(dq), torch.isnan(want)) and torch.equal(torch.isinf(dq), torch.isinf(want))
