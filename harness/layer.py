@@ -47,6 +47,7 @@ class LayerAttention:
         slots = c.Kl[:, at * c.nqb:(at + 1) * c.nqb].view(c.H, c.nqb * c.B, c.d)[None, :, :c.Nq]
         qt, kt = q[None].transpose(1, 2), k[None].transpose(1, 2)
         p = layer.make_rotary(qt, kt, self.q[None], slots, sections=self.sections, mscale=self.mscale)
+        torch.autograd.graph.increment_version([c.Kl])         # as an append would, so that a backward which saved the ring notices
         layer.pbsa_norm_rotate_fwd(p, qt, kt, self.wq, self.wk, pos, self.freq, self.q[None], slots)
         c.adopt_chunk(chunk_id)
         c.rewrite_chunk(V=v.transpose(0, 1))
@@ -69,7 +70,8 @@ class LayerAttention:
 
     def train(self, q, k, v, qc, pos, chunk_id, gradient):
         """A step with gradients; gradient(o, cross) gives those of the two outputs.  Returns the outputs and the gradients of q, k,
-        v, qc, the norms' weights and the prompt's states; what earlier chunks contributed stays in the cache's gradients."""
+        v, qc, the norms' weights and the prompt's states.  They end at the chunk: what its attention owes to the keys and values of
+        earlier ones, in the window, the slots or the summary, is left out."""
         c = self.cache
         self._append(q, k, v, pos, chunk_id)
         c.select(self.q)

@@ -71,3 +71,18 @@ def test_gradients_of_the_first_chunk():
     assert off(o, want_o) < 2.0 ** -7 and off(cross, want_c) < 2.0 ** -7
     for n, y in leaves.items():
         assert off(got[n], y.grad) < 2.0 ** -6, n
+
+
+def test_a_backward_that_saved_the_ring_notices_a_step():
+    """As with an append of the cache's own: what autograd saved of the keys or the values is known to have changed."""
+    H, d, B, Nq, w, C, k, _ = GEOMETRY
+    for name in ("Kl", "Vl"):
+        one, g = made()
+        ring = getattr(one.cache, name)
+        x = torch.ones(d, device=DEV, requires_grad=True)
+        with torch.enable_grad():
+            y = (ring.float() * 1).mul(x).sum() + (ring * x.bfloat16()).float().sum()      # saves the ring itself
+        q, kk, v, qc = example.random_chunk(one, g)
+        one.step(q, kk, v, qc, example.frame_positions(Nq, (5, 8), 0, DEV), 0)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
