@@ -94,7 +94,8 @@ typedef struct pbsa_cross {
   int64_t dO[3], dq[3], dk[3], dv[3];      /* backward only                                         */
 } pbsa_cross;
 
-/* ws: pbsa_cross_workspace_bytes(p) bytes of scratch, 256-byte aligned (0 where the call needs none: then ws may be NULL). */
+/* Rows of all heads from 2^29 on are refused (PBSA_ESHAPE) under a mask if the last state lies 4 GiB or more behind the first.
+ * ws: pbsa_cross_workspace_bytes(p) bytes of scratch, 256-byte aligned (0 where the call needs none: then ws may be NULL). */
 int pbsa_cross_workspace_bytes(const pbsa_cross* p, size_t* out);
 int pbsa_cross_attention_fwd(const pbsa_cross* p, const void* Q, const void* K, const void* V, const int32_t* k_len,
                              const uint8_t* k_mask, void* O, float* lse, void* ws, size_t ws_bytes, void* hip_stream);

@@ -892,6 +892,13 @@ hipError_t launch_typed(const CrossShape& s, const CrossArgs& a, int n, hipStrea
 
 }  // namespace
 
+// A launch holds fewer than 2^32 threads.  Rows in units of 128 always fit (the checks count 2^30 of them), and so do up to four rows to
+// a head; units of 32, which few rows take and masked states far apart, may not.
+bool cross_fits(const pbsa_cross& p, bool masked) {
+  const CrossShape s = cross_shape(p, masked);
+  return (s.units * s.parts + 7) / 8 * 8 * 64 * s.waves < (int64_t)1 << 32;
+}
+
 size_t cross_workspace_bytes(const pbsa_cross& p, bool masked) {
   const CrossShape s = cross_shape(p, masked);
   if (s.by == By::rows) return masked ? attended_bytes(p.n, p.Nk) : 0;

@@ -181,6 +181,7 @@ int pbsa_cross_attention_fwd(const pbsa_cross* p, const void* Q, const void* K, 
   if (rc || (rc = check_cross_inputs(p, Q, K, V, k_len, k_mask))) return rc;
   if ((rc = check_view({O, p->o, p->n, p->Hq, p->T, true}, p->d))) return rc;
   if (!aligned(lse, 4)) return PBSA_EALIGN;
+  if (!pbsa::cross_fits(*p, k_mask != nullptr)) return PBSA_ESHAPE;
   if ((rc = check_scratch(ws, ws_bytes, pbsa::cross_workspace_bytes(*p, k_mask != nullptr)))) return rc;
   return pbsa::report(pbsa::launch_cross(*p, Q, K, V, k_len, k_mask, O, lse, ws, static_cast<hipStream_t>(hip_stream)));
 }

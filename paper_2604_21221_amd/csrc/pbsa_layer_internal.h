@@ -27,7 +27,7 @@ struct RotaryTensors {
 size_t rotary_workspace_bytes(const pbsa_rotary& p);
 hipError_t launch_rotary(const pbsa_rotary& p, RotaryOp op, const RotaryTensors& t, void* ws, hipStream_t stream);
 
-
+bool cross_fits(const pbsa_cross& p, bool masked);   // into a launch
 size_t cross_workspace_bytes(const pbsa_cross& p, bool masked);
 // The attended states of each sequence under a mask, in order: counts [n] in the first attended_first(n) places of the scratch,
 // the list [n][Nk] behind them (pbsa_cross_list.hip).

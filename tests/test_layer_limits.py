@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2604_21221_amd import layer, pbsa  # noqa: E402
-from tests.test_layer_abi import cross  # noqa: E402
+from tests.test_layer_abi import A, ESHAPE, EWS, cross, cross_fwd, refused  # noqa: E402
 
 LOAD = 240 + 3 * 1024    # bytes that a load of the list kernel adds to its state's offset: a chunk of the row, its place among four
 
@@ -38,3 +38,11 @@ def test_offsets_of_listed_states_stay_within_32_bits(d, step):
             assert (Nk - 1) * 2 * step + LOAD + 16 <= 1 << 32, Nk
     far = (1 << 32) // (2 * step) // 2                       # halfway there is nothing to be careful about
     assert by_list(d, far, step)
+
+
+def test_more_rows_than_a_launch_takes_are_refused():
+    """Masked states that lie too far apart for a list go by units of 32 rows, 256 threads to each."""
+    for T, Hq in ((1 << 30, 1), ((1 << 29) + 32, 1), (1 << 22, 256)):
+        refused(ESHAPE, cross_fwd, cross(n=1, T=T, Nk=129, Hq=Hq, Hk=1, d=64, k=(0, 0, 1 << 24), q=(0, 0, 0), o=(0, 64 * T, 64)), k_mask=A)
+    # half as many go on to the next check
+    refused(EWS, cross_fwd, cross(n=1, T=40, Nk=1 << 14, Hq=1, Hk=1, d=64, k=(0, 0, 1 << 24)), k_mask=A, ws=None)
