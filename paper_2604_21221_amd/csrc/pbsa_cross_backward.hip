@@ -130,6 +130,7 @@ __device__ __forceinline__ s16x8 operand_of(const uint32_t* p) {
 // kFewStates, however many it has room for, the sum itself is formed, in binary32.  Error of dQ and dK in bf16, of their norm, with two states 0.0050 by the outputs, 0.0023
 // by the sum; eight 0.0033 and 0.0024; sixteen 0.0030 and 0.0024.  Time with three, 5 x 8676 rows of 15 heads of 64: 167 us and
 // 187; with ten, 5 x 316 of 14 of 128: 26 and 37.
+// With one state P = 1 and dP = delta: dS is zero, and is made so.
 constexpr int kFewStates = 8;
 // Those of a mask, in order, by a wave: their number if there are up to kFewStates, else more than that.  Whole waves of a workgroup
 // may do so with the same `few` in LDS: they write the same.  Mostly the first 64 states tell; else 1024 to a turn, bound by latency.
@@ -448,6 +449,7 @@ __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* r
     a.stat_delta[(int64_t)bh * a.row_tiles * 128 + m] = on ? w.delta : 0.0f;
   }
   const float k = kLift ? lift(top) : 0.0f;
+  if (states.count == 1) w.lse = INFINITY;
   w.lse += k;
   float* const tops = reinterpret_cast<float*>(ring + 2 * Z::kTile);         // (no tile is there yet)
   if constexpr (kLift && STATS) {
@@ -820,8 +822,8 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
 
   const Attended keys = attended_of(a.k_len, a.k_mask, a.mask_stride_b, b, a.Nk);
   const int m_end = min(a.M, (part + 1) * a.part_rows), len = keys.len;
-  const int32_t* const list = OWN && a.list ? a.list + b * a.Nk : nullptr;
-  const int count = OWN && a.list ? __builtin_amdgcn_readfirstlane(a.counts[b]) : len;   // of attended states
+  const int32_t* const list = a.list ? a.list + b * a.Nk : nullptr;
+  const int count = a.list ? __builtin_amdgcn_readfirstlane(a.counts[b]) : len;          // of attended states
   const uint32_t on_bits = (uint32_t)keys.bits<32>(key0, lane);
   const bool on = on_bits >> (lane & 31) & 1;
   // a tile past the sequence's states has nothing to add up
@@ -1007,7 +1009,8 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
       settle(w.dv[dt]);
     }
   }
-  const bool again = kLift && beyond(w.dk[0][0], on && top < INFINITY);
+  if (count == 1) unlift = 0.0f;
+  const bool again = kLift && beyond(w.dk[0][0], on && top < INFINITY && count != 1);
   const auto plain = [&](f32x4* to) {
     if constexpr (kLift) {
       if (__builtin_expect(again, 0)) {
@@ -1173,7 +1176,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) cross_grad_few_kernel(CrossGra
         s = over_row<LPK>(s);
         dp = over_row<LPK>(dp);
         const float p = on[u] ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, a.c2, -lse[r])) : 0.0f;
-        const float ds = on[u] ? p * (dp - delta[r]) * a.scale : 0.0f;
+        const float ds = on[u] && count != 1 ? p * (dp - delta[r]) * a.scale : 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           dq[r][e] = __builtin_fmaf(ds, kf[e], dq[r][e]);
