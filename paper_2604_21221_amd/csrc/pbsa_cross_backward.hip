@@ -12,12 +12,13 @@
 //   cross_grad_few_kernel  up to four rows: everything in one pass over the states
 // Rows are those of all query heads that share a head of K and V (m = t G + g), which sums their gradients as it goes.
 //
-// P and dS are rounded to the tensors' type as operands: with the outputs' own rounding, sqrt 2 times the error of that alone.
+// P and dS are rounded to the tensors' type as operands: with the outputs' own rounding, sqrt 2 times the error of that alone; delta
+// from a rounded O adds to it (sum_delta).
 // In fp16 the gradients of the scores can lie far below what it holds normally (they are dO over the number of states), so dS is
 // formed times 2^-k, k by the largest |dO|, of the row for dQ and of the workgroup's rows for dK; 2^-k goes into the exponent of P.
 //
-// Measured, 4680 x 512 x 12 x 128 in bf16: dQ 37.6 us (22 GFLOP; 8.6 us until the rows are there, 43 MB; 18 us of steps, 1.2
-// PFLOP/s, a large library product's rate), dK and dV 37.1 (29 GFLOP; 25 us of steps), their join 6.8 (31 MB).  With all
+// Measured, 4680 x 512 x 12 x 128 in bf16: dQ 37.5 us (22 GFLOP; 8.6 us until the rows are there, 43 MB; 18 us of steps, 1.2
+// PFLOP/s, a large library product's rate), dK and dV 37.8 (29 GFLOP; 25 us of steps), their join 6.6 (31 MB).  With all
 // workgroups in one round, first loads and last stores have nothing beside them.
 #include <algorithm>
 

@@ -12,8 +12,8 @@
 // would move more bytes than the positions, and the table would have to reach to the farthest of them).
 //
 // Measured, at 21504 x 12 x 128 of two tensors, 265 MB: 53 us, 5.0 TB/s (a copy of 1 GiB: 5.15).  At 4680 x 12 x 128 with the norm,
-// 58 MB: 13.0 us; its backward, 86 MB: 20.6 us and 4.5 for the sum of the workgroups' shares of the weights' gradients: there
-// a third of the time is launch and first loads, and the backward's 350 instructions for a row of a lane are another.
+// 58 MB: 12.6 us; its backward, 86 MB: 19 us and 3.2 for the sum of the workgroups' shares of the weights' gradients: there
+// a third of the time is launch and first loads, and the backward's 360 instructions for a row of a lane are another.
 #include <algorithm>
 
 #include "pbsa_layer_internal.h"
