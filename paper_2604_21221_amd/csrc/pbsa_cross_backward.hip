@@ -68,7 +68,7 @@ __device__ __forceinline__ int place(int bx, int n) {
 // k of 2^-k for gradients of at most `top`, which are below 1 by it: |dS| = P |dP - sum P dP| is at most P (1 - P) times how far
 // two of dO V^T lie apart, half the sum of |V| over d, and fp16 holds it as long as that sum is below 2^17.  Where it does not, the
 // wave forms its sums again in binary32 (dq_plain, dk_plain): without matrix instructions, a matter of being right (4680 x 512 x 12 of
-// 128 with every wave doing so: 5.4 ms).
+// 128 with nearly every wave doing so: 5.7 ms).
 __device__ __forceinline__ float lift(float top) {
   if (!(top > 0.0f) || !(top < INFINITY)) return 0.0f;
   return fminf(fmaxf((float)__builtin_amdgcn_frexp_expf(top), -60.0f), 60.0f);
@@ -104,6 +104,8 @@ __device__ __forceinline__ float over_row(float v) {
   return v;
 }
 
+// Whether a row's gradients are infinite or NaN anyhow, of which nothing can be made by summing up again: it counts as one of infinite dO.
+__device__ __forceinline__ bool lost(float lse, float delta) { return !(fabsf(delta) < INFINITY) || lse != lse; }
 // Whether dS of a wave's has been infinite in a column that counts: then all of the column's sums are infinite or NaN, and one tells.
 __device__ __forceinline__ bool beyond(float sum, bool counts) { return __any(counts && !(fabsf(sum) < INFINITY)); }
 template <typename E>
@@ -450,6 +452,7 @@ __device__ __forceinline__ void dq_part(const CrossGradArgs& a, unsigned char* r
     a.stat_delta[(int64_t)bh * a.row_tiles * 128 + m] = on ? w.delta : 0.0f;
   }
   const float k = kLift ? lift(top) : 0.0f;
+  if (kLift && lost(w.lse, w.delta)) top = INFINITY;
   if (states.count == 1) w.lse = INFINITY;
   w.lse += k;
   float* const tops = reinterpret_cast<float*>(ring + 2 * Z::kTile);         // (no tile is there yet)
@@ -909,6 +912,7 @@ __device__ __forceinline__ void dkv_part(const CrossGradArgs& a, unsigned char* 
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
+          if (kLift && lost(lse[u], delta[u])) top = INFINITY;
           if (lane % T::CH == 0) {
             float* const to = stat + 2 * kRows * i + row_of_load(u);
             to[0] = lse[u] - lift_p<E>();
